@@ -12,11 +12,11 @@ namespace ug {
 struct ChunkBatch {
   const int32_t *cu, *lens, *table;
   int S, num_rows, max_blocks, num_blocks;
-  __device__ __forceinline__ int rows(int b, int& row0) const {
+  __host__ __device__ __forceinline__ int rows(int b, int& row0) const {
     row0 = min(max(cu[b], 0), num_rows);
-    return max(min(cu[b + 1], num_rows) - row0, 0);
+    return max(min(cu[b + 1], num_rows), row0) - row0;  // (in this order: an end near the least int has no difference to row0)
   }
-  __device__ __forceinline__ int len(int b) const { return min(max(lens[b], 0), max_blocks * UNIGIST_PAGE_TOKENS); }
+  __host__ __device__ __forceinline__ int len(int b) const { return min(max(lens[b], 0), max_blocks * UNIGIST_PAGE_TOKENS); }
   __device__ __forceinline__ int page(int b, int i) const {  // i < max_blocks
     return min(max(table[(long long)b * max_blocks + i], 0), num_blocks - 1);
   }
