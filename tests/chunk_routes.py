@@ -10,8 +10,8 @@ from chunk_util import Cache
 
 # name: (kernels launched, query heads, KV heads, head size, pages of a table row, tokens per sequence that fit the route)
 ROUTES = {
-    "rows64": (["chunk_attn_sm100_kernel", "chunk_combine_kernel"], 8, 2, 64, 12, 40),
-    "rows128": (["chunk_attn_sm100_kernel", "chunk_combine_kernel"], 8, 2, 128, 12, 40),
+    "rows64": (["chunk_attn_sm100_kernel", "chunk_combine_kernel"], 8, 2, 64, 60, 40),
+    "rows128": (["chunk_attn_sm100_kernel", "chunk_combine_kernel"], 8, 2, 128, 60, 40),
     "clusters64": (["chunk_few_kernel"], 8, 2, 64, 12, 4),
     "clusters128": (["chunk_few_kernel"], 8, 2, 128, 12, 4),
     "shares64": (["chunk_few_kernel", "chunk_combine_kernel"], 8, 2, 64, 400, 4),
@@ -34,9 +34,12 @@ def launched(call):
 def cache_of(route, lens, seed=0, **kw):
     """A cache whose table is as wide as the route wants it: the entries behind a sequence's pages name no page."""
     _, _, hkv, dim, width, _ = ROUTES[route]
-    cache = Cache(lens, hkv, dim, seed=seed, **kw)
-    assert cache.width <= width, "the sequences outgrow the route's table"
-    wide = torch.full((len(lens), width), -7, dtype=torch.int32)
+    return widened(Cache(lens, hkv, dim, seed=seed, **kw), width)
+
+
+def widened(cache, width):
+    assert cache.width <= width, "the sequences outgrow the table"
+    wide = torch.full((len(cache.lens), width), -7, dtype=torch.int32)
     wide[:, ::2] = 2 ** 30
     wide[:, : cache.width] = cache.table
     cache.table, cache.width = wide, width
