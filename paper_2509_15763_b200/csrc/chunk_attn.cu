@@ -80,10 +80,10 @@ __device__ __forceinline__ float half_max(const uint32_t (&sc)[kHalf]) {
   float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
   for (int e = 0; e < kHalf; e += 4) {
-    m0 = max3(m0, __uint_as_float(sc[e]), __uint_as_float(sc[e + 1]));
-    m1 = max3(m1, __uint_as_float(sc[e + 2]), __uint_as_float(sc[e + 3]));
+    m0 = max3<true>(m0, __uint_as_float(sc[e]), __uint_as_float(sc[e + 1]));
+    m1 = max3<true>(m1, __uint_as_float(sc[e + 2]), __uint_as_float(sc[e + 3]));
   }
-  return fmaxf(m0, m1);
+  return max2<true>(m0, m1);
 }
 __device__ __forceinline__ float half_exp(const uint32_t (&sc)[kHalf], uint32_t t_p, float scale_log2, float m) {
   uint64_t l01 = f32x2(0.f, 0.f), l23 = l01;
@@ -422,10 +422,16 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           ++cnt;
           continue;
         }
+        // A score that is NaN or without end leaves the row none: with a NaN for its maximum all of its weights are NaN.  (The weights
+        // alone would not show it: those on the FMA pipe are numbers whatever comes in.)
+        auto maximum = [&](float mx) {
+          const float mx_s = mx * P.scale_log2;
+          return mx_s < INFINITY ? mx_s : __int_as_float(0x7fffffff);
+        };
         // Some row of this warp outgrew its running maximum: O is rescaled, and the exponentials are to be taken again.
         auto outgrown = [&](float mx) {
-          const float mx_s = mx * P.scale_log2;
-          const bool need = mx_s > m_run + kRescaleThreshold;
+          const float mx_s = maximum(mx);
+          const bool need = !(mx_s <= m_run + kRescaleThreshold);
           if (!__any_sync(0xffffffffu, need)) return false;
           const float m_new = need ? mx_s : m_run;
           const float f = need ? ex2(m_run - m_new) : 1.f;  // m_run = -inf gives 0
@@ -456,7 +462,7 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           if (c0 + kHalf - 1 > hi_all) half_mask(sc, hi_row - c0);
           // (the maximum first: kept for another pass, the scores would not fit the registers)
           mx = half_max(sc);
-          if (cnt == 0) m_run = mx * P.scale_log2;
+          if (cnt == 0) m_run = maximum(mx);
           else outgrown(mx);
           tile_sum = half_exp(sc, tS, P.scale_log2, m_run == -INFINITY ? 0.f : m_run);
         } else {
@@ -465,9 +471,9 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           for (int c = 0; c < kCols / 32; ++c) tmem_ld32(tS + c * 32, sc + c * 32);
           tmem_wait_ld();
           if (col0 + BN - 1 > hi_all) mask_row(sc, 0, hi_row - col0);
-          if (cnt == 0) m_run = row_max(sc) * P.scale_log2;
+          if (cnt == 0) m_run = maximum(row_max<true>(sc));
           for (int pass = 0; pass < 2; ++pass) {
-            tile_sum = row_exp<0>(sc, tS, P.scale_log2, m_run == -INFINITY ? 0.f : m_run, mx);
+            tile_sum = row_exp<0, true>(sc, tS, P.scale_log2, m_run == -INFINITY ? 0.f : m_run, mx);
             if (!outgrown(mx)) break;
           }
           tmem_wait_st();
@@ -504,7 +510,7 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         if (!whole)
           P.part_ml[slot * P.slot_rows + (single ? 0 : i * BM) + r] = make_float2(m, l);
         else if (P.lse)
-          P.lse[out_row(r)] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+          P.lse[out_row(r)] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
       };
       // Streams that hold sums of this tile's rows (of a single tile's one step those of tile 1 had none).
       const int joined = single && x.j1 - x.j0 > 1 ? 2 * kHalves : kHalves;
@@ -532,7 +538,7 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
           f = m_run == -INFINITY ? 0.f : ex2(m_run - m), f_other = y.x == -INFINITY ? 0.f : ex2(y.x - m);
           l = l_run * f + y.y * f_other;
         }
-        const float inv_l = l > 0.f ? 1.f / l : 0.f;
+        const float inv_l = l != 0.f ? 1.f / l : 0.f;  // (a NaN stays one)
         if (whole) f *= inv_l, f_other *= inv_l;
 #pragma unroll 1
         for (int c = half; c < (kHalves == 2 ? half + 1 : D / 32) && mine; ++c) {
@@ -548,8 +554,8 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             }
             // (the sums of a stream that has seen nothing of the row are not worth reading)
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) v[e] = f > 0.f ? __float_as_uint(__uint_as_float(v[e]) * f) : 0u;
-            if (kHalves == 2 && f_other > 0.f) {
+            for (int e = 0; e < kPiece; ++e) v[e] = f != 0.f ? __float_as_uint(__uint_as_float(v[e]) * f) : 0u;
+            if (kHalves == 2 && f_other != 0.f) {
               const float4* y = reinterpret_cast<const float4*>(gen + SM::kOffStage + st * 16384 + p * 512 + r * 16);
 #pragma unroll
               for (int e = 0; e < kPiece; e += 4) {
@@ -605,7 +611,7 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         }
         named_barrier_sync(kBar, kSumThreads);
         float f = m_run == -INFINITY ? 0.f : ex2(m_run - M);
-        if (whole) f *= l > 0.f ? 1.f / l : 0.f;
+        if (whole) f *= l != 0.f ? 1.f / l : 0.f;
         if (st == 0) leave_stats(M, l);
 #pragma unroll 1
         for (int c0 = 0; c0 < D; c0 += cols) {
@@ -615,7 +621,7 @@ chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
             tmem_ld32(tO + c0 + c, v);
             tmem_wait_ld();
             // (the sums of a stream that has seen nothing of the row are not worth reading)
-            auto weighed = [&](int e) { return f > 0.f ? __float_as_uint(__uint_as_float(v[e]) * f) : 0u; };
+            auto weighed = [&](int e) { return f != 0.f ? __float_as_uint(__uint_as_float(v[e]) * f) : 0u; };
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
               st_shared_v4(base + SM::kOffStage + (((st * room_rows + r) * chunks + (((c + e) >> 2) ^ (r & 7))) << 4),
@@ -688,6 +694,7 @@ chunk_combine_kernel(const __grid_constant__ ChunkParams P) {
   __syncthreads();
   if (!real) return;
   float M = -INFINITY, sum = 0.f;
+  bool none = false;  // some part holds a score that is no number
   float4 acc[kVecs];
 #pragma unroll
   for (int q = 0; q < kVecs; ++q) acc[q] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -707,7 +714,7 @@ chunk_combine_kernel(const __grid_constant__ ChunkParams P) {
     }
     float m = M;
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) m = fmaxf(m, ml[u].x);
+    for (int u = 0; u < kLoads; ++u) m = fmaxf(m, ml[u].x), none |= ml[u].y != ml[u].y;
     if (m == -INFINITY) continue;  // nothing seen so far
     const float f = ex2(M - m);
     M = m;
@@ -725,15 +732,16 @@ chunk_combine_kernel(const __grid_constant__ ChunkParams P) {
     }
   }
   const long long out = (long long)(head.row0 + tok) * P.Hq + head.hk * P.G + (r - (tok - tile * P.tpt) * P.G);
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  if (none) sum = __int_as_float(0x7fffffff);
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
   uint2 pk[kVecs];
 #pragma unroll
   for (int q = 0; q < kVecs; ++q)
-    pk[q] = sum > 0.f ? make_uint2(pack_bf16(acc[q].x * inv, acc[q].y * inv), pack_bf16(acc[q].z * inv, acc[q].w * inv)) : make_uint2(0u, 0u);
+    pk[q] = sum != 0.f ? make_uint2(pack_bf16(acc[q].x * inv, acc[q].y * inv), pack_bf16(acc[q].z * inv, acc[q].w * inv)) : make_uint2(0u, 0u);
 #pragma unroll
   for (int q = 0; q < kVecs; q += 2)
     *reinterpret_cast<uint4*>(P.o + out * D + (warp * kVecs + q) * 4) = make_uint4(pk[q].x, pk[q].y, pk[q + 1].x, pk[q + 1].y);
-  if (P.lse && warp == 0) P.lse[out] = sum > 0.f ? (M + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+  if (P.lse && warp == 0) P.lse[out] = sum != 0.f ? (M + log2f(sum)) * 0.6931471805599453f : -INFINITY;
 }
 
 // Blocks of a call: no more than there can be steps.

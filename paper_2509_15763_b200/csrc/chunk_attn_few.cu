@@ -269,7 +269,8 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
       if (qc == 0) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) ml[stage * F::kRows + mt * 16 + r * 8 + g] = make_float2(m_run[r], l_run[r]);
+        for (int r = 0; r < 2; ++r)  // (scores that are NaN pass the maximum by; what the warps add up goes by it, so it becomes one too)
+          ml[stage * F::kRows + mt * 16 + r * 8 + g] = make_float2(l_run[r] == l_run[r] ? m_run[r] : l_run[r], l_run[r]);
       }
       if constexpr (!kFlat) {
         // The warps' results lie in the ring, each in its own stage, [row][D] fp32 in 16-byte pieces whose place turns with the row;
@@ -311,10 +312,10 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             reinterpret_cast<float4*>(gen)[piece(row, d4)] = acc;
             if (d4 == 0) merged[row] = make_float2(M, L);
           } else if (ok) {
-            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const float inv = L != 0.f ? 1.f / L : 0.f;
             const long long out = out_row(row);
             *reinterpret_cast<uint2*>(P.o + out * D + 4 * d4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-            if (P.lse && d4 == 0) P.lse[out] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+            if (P.lse && d4 == 0) P.lse[out] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
           }
         }
         cluster_sync();
@@ -334,10 +335,10 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
               acc.x += w * y.x, acc.y += w * y.y, acc.z += w * y.z, acc.w += w * y.w;
               L += w * ld_cluster_f32(ml_at + 4, k);
             }
-            const float inv = L > 0.f ? 1.f / L : 0.f;
+            const float inv = L != 0.f ? 1.f / L : 0.f;
             const long long out = out_row(row);
             *reinterpret_cast<uint2*>(P.o + out * D + 4 * d4) = make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
-            if (P.lse && d4 == 0) P.lse[out] = L > 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
+            if (P.lse && d4 == 0) P.lse[out] = L != 0.f ? (M + log2f(L)) * kLn2 : -INFINITY;
           }
         }
         fence_proxy_async_smem();  // (what follows in the ring is written by the other proxy)
@@ -396,11 +397,11 @@ chunk_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             if (row >= rows) continue;
             if (whole) {
               const long long out = out_row(row);
-              const float inv = l > 0.f ? 1.f / l : 0.f;
+              const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
               for (int d = 0; d < D / 8; ++d)
                 *reinterpret_cast<uint32_t*>(P.o + out * D + 8 * d + 2 * qc) = pack_bf16(o[d][2 * r] * inv, o[d][2 * r + 1] * inv);
-              if (P.lse && qc == 0) P.lse[out] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+              if (P.lse && qc == 0) P.lse[out] = l != 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
             } else {
 #pragma unroll
               for (int d = 0; d < D / 8; ++d)

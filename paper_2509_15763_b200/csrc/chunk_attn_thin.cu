@@ -342,16 +342,16 @@ chunk_thin_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
       }
       // of row `lane`: the sum of its weights, and what its outputs are multiplied by
       const float my_sum = (wmax[lane] + wmax[NQ + lane]) + (wmax[2 * NQ + lane] + wmax[3 * NQ + lane]);
-      const float my_inv = my_sum > 0.f ? 1.f / my_sum : 0.f;
+      const float my_inv = my_sum != 0.f ? 1.f / my_sum : 0.f;  // (a NaN stays one)
       float my_m = -INFINITY;
 #pragma unroll
       for (int q = 0; q < NQ; ++q) my_m = q == lane ? m[q] : my_m;
       if (ok && lane < rows && warp == 0) {
         const int tok = fdiv(P.g_div, lane);
         if (!whole)
-          P.part_ml[slot * P.slot_rows + lane] = make_float2(my_sum > 0.f ? my_m : -INFINITY, my_sum);
+          P.part_ml[slot * P.slot_rows + lane] = make_float2(my_sum != 0.f ? my_m : -INFINITY, my_sum);
         else if (P.lse)
-          P.lse[(long long)(x.row0 + tok) * P.Hq + x.hk * P.G + (lane - tok * P.G)] = my_sum > 0.f ? (my_m + log2f(my_sum)) * 0.6931471805599453f : -INFINITY;
+          P.lse[(long long)(x.row0 + tok) * P.Hq + x.hk * P.G + (lane - tok * P.G)] = my_sum != 0.f ? (my_m + log2f(my_sum)) * 0.6931471805599453f : -INFINITY;
       }
       if (ok && whole) {
         __nv_bfloat16* to = P.o + ((long long)x.row0 * P.Hq + x.hk * P.G) * D + key;
@@ -360,7 +360,7 @@ chunk_thin_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
         for (int q = 0; q < NQ; ++q) {
           if (q >= rows) break;
           const float inv = __shfl_sync(0xffffffffu, my_inv, q);
-          *to = __float2bfloat16_rn(inv > 0.f ? __uint_as_float(o[q]) * inv : 0.f);
+          *to = __float2bfloat16_rn(inv != 0.f ? __uint_as_float(o[q]) * inv : 0.f);
           const bool last = ++g == P.G;  // of the token
           to += last ? (long long)(P.Hq - P.G + 1) * D : D;
           g = last ? 0 : g;
@@ -370,7 +370,7 @@ chunk_thin_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_c
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
           if (q >= rows) break;
-          to[4 * q] = __shfl_sync(0xffffffffu, my_inv, q) > 0.f ? __uint_as_float(o[q]) : 0.f;
+          to[4 * q] = __shfl_sync(0xffffffffu, my_inv, q) != 0.f ? __uint_as_float(o[q]) : 0.f;
         }
       }
       named_barrier_sync(2, 128);  // the sums have been read

@@ -10,10 +10,19 @@ using namespace sm100;
 
 constexpr int kCols = 128;  // score columns per thread and tile
 
+// kNan: a NaN among them is the maximum.
+template <bool kNan = false>
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  if constexpr (kNan)
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  else
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+template <bool kNan = false>
+__device__ __forceinline__ float max2(float a, float b) {
+  return kNan ? max3<true>(a, b, b) : fmaxf(a, b);
 }
 
 // Bit e of the result: column 32 * c + e lies inside [lo, hi].
@@ -33,16 +42,17 @@ __device__ __forceinline__ void mask_row(uint32_t (&sc)[kCols], int lo, int hi) 
 }
 
 // Row maximum of the raw scores of one tile.
+template <bool kNan = false>
 __device__ __forceinline__ float row_max(const uint32_t (&sc)[kCols]) {
   float m0 = -INFINITY, m1 = -INFINITY, m2 = -INFINITY, m3 = -INFINITY;
 #pragma unroll
   for (int e = 0; e < kCols; e += 8) {
-    m0 = max3(m0, __uint_as_float(sc[e]), __uint_as_float(sc[e + 1]));
-    m1 = max3(m1, __uint_as_float(sc[e + 2]), __uint_as_float(sc[e + 3]));
-    m2 = max3(m2, __uint_as_float(sc[e + 4]), __uint_as_float(sc[e + 5]));
-    m3 = max3(m3, __uint_as_float(sc[e + 6]), __uint_as_float(sc[e + 7]));
+    m0 = max3<kNan>(m0, __uint_as_float(sc[e]), __uint_as_float(sc[e + 1]));
+    m1 = max3<kNan>(m1, __uint_as_float(sc[e + 2]), __uint_as_float(sc[e + 3]));
+    m2 = max3<kNan>(m2, __uint_as_float(sc[e + 4]), __uint_as_float(sc[e + 5]));
+    m3 = max3<kNan>(m3, __uint_as_float(sc[e + 6]), __uint_as_float(sc[e + 7]));
   }
-  return fmaxf(fmaxf(m0, m1), fmaxf(m2, m3));
+  return max2<kNan>(max2<kNan>(m0, m1), max2<kNan>(m2, m3));
 }
 
 // Half a pass over a row of raw scores (columns 64 * kHalf .. + 63): p = 2^(s * scale_log2 - m) written to
@@ -52,7 +62,7 @@ __device__ __forceinline__ float row_max(const uint32_t (&sc)[kCols]) {
 // pipe).  The special-function unit (16 exponentials per clock and SM) bounds this loop, so kEmuNum of every
 // kEmuDen column pairs go to the FMA pipe (ex2_fma2) and the maximum rides along on the ALU pipe.
 constexpr int kEmuNum = 2, kEmuDen = 8;
-template <int kHalf>
+template <int kHalf, bool kNan = false>
 __device__ __forceinline__ float row_exp(const uint32_t (&sc)[kCols], uint32_t t_p, float scale_log2, float m, float& mx) {
   uint64_t l01 = f32x2(0.f, 0.f), l23 = l01;
   const uint64_t scale2 = f32x2(scale_log2, scale_log2), negm2 = f32x2(-m, -m);
@@ -78,10 +88,10 @@ __device__ __forceinline__ float row_exp(const uint32_t (&sc)[kCols], uint32_t t
       }
       if (kHalf == 0) {  // the maximum of both halves: 8 columns per 4 exponentials
         const int j0 = 2 * i0;
-        m0 = max3(m0, __uint_as_float(sc[j0]), __uint_as_float(sc[j0 + 1]));
-        m1 = max3(m1, __uint_as_float(sc[j0 + 2]), __uint_as_float(sc[j0 + 3]));
-        m0 = max3(m0, __uint_as_float(sc[j0 + 4]), __uint_as_float(sc[j0 + 5]));
-        m1 = max3(m1, __uint_as_float(sc[j0 + 6]), __uint_as_float(sc[j0 + 7]));
+        m0 = max3<kNan>(m0, __uint_as_float(sc[j0]), __uint_as_float(sc[j0 + 1]));
+        m1 = max3<kNan>(m1, __uint_as_float(sc[j0 + 2]), __uint_as_float(sc[j0 + 3]));
+        m0 = max3<kNan>(m0, __uint_as_float(sc[j0 + 4]), __uint_as_float(sc[j0 + 5]));
+        m1 = max3<kNan>(m1, __uint_as_float(sc[j0 + 6]), __uint_as_float(sc[j0 + 7]));
       }
       l01 = add2(l01, f32x2(x[0], x[1]));
       l23 = add2(l23, f32x2(x[2], x[3]));
@@ -90,7 +100,7 @@ __device__ __forceinline__ float row_exp(const uint32_t (&sc)[kCols], uint32_t t
     }
     tmem_st(t_p + c * 16, pk);
   }
-  if (kHalf == 0) mx = fmaxf(m0, m1);
+  if (kHalf == 0) mx = max2<kNan>(m0, m1);
   float l0, l1, l2, l3;
   f32x2_split(l01, l0, l1);
   f32x2_split(l23, l2, l3);
