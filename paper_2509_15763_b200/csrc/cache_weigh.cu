@@ -142,10 +142,17 @@ struct Share {
 
 // 2^x for two values on the FMA pipe: x = n + f with n = round(x) (taken from the low mantissa bits of x + 1.5 * 2^23), 2^f on
 // [-0.5, 0.5] by the polynomial of degree 5 of least relative error (Remez' exchange; 2.1e-7 as evaluated, what ex2.approx
-// leaves too), n added to the exponent field.  Below -126 about 2^-126 instead of 0, above 127.99 2^127.99 instead of infinity.
+// leaves too), times 2^n.  Below -126 about 2^-126 instead of 0, above 127.49 2^127.49 instead of infinity; a NaN stays one (which it
+// would not with n added to the exponent field of a NaN).
+__device__ __forceinline__ float clamp_nan(float x, float lo, float hi) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(x), "f"(lo));
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(d), "f"(hi));
+  return d;
+}
 __device__ __forceinline__ void ex2_fma2_deg5(float& x0, float& x1) {
   const uint64_t magic = f32x2(12582912.f, 12582912.f);
-  const uint64_t x = f32x2(fminf(fmaxf(x0, -126.f), 127.99f), fminf(fmaxf(x1, -126.f), 127.99f));
+  const uint64_t x = f32x2(clamp_nan(x0, -126.f, 127.49f), clamp_nan(x1, -126.f, 127.49f));
   const uint64_t t = add2(x, magic);
   const uint64_t f = sub2(x, sub2(t, magic));
   uint64_t p = fma2(f, f32x2(0.00132764725f, 0.00132764725f), f32x2(0.00967554096f, 0.00967554096f));
@@ -153,11 +160,10 @@ __device__ __forceinline__ void ex2_fma2_deg5(float& x0, float& x1) {
   p = fma2(p, f, f32x2(0.240221202f, 0.240221202f));
   p = fma2(p, f, f32x2(0.693146944f, 0.693146944f));
   p = fma2(p, f, f32x2(1.00000012f, 1.00000012f));
-  float t0, t1, p0, p1;
+  float t0, t1;
   f32x2_split(t, t0, t1);
-  f32x2_split(p, p0, p1);
-  x0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-  x1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+  auto pow2 = [](float t) { return __uint_as_float((__float_as_uint(t) << 23) + 0x3f800000u); };
+  f32x2_split(mul2(p, f32x2(pow2(t0), pow2(t1))), x0, x1);
 }
 
 // The special-function unit (16 exponentials a clock and SM) bounds a chunk's sums, so kEmuNum of every 8 column pairs that

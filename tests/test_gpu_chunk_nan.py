@@ -1,4 +1,5 @@
-"""A score that is no number shows in what it reaches, and nowhere else: the query's output and log-sum-exp.  (Zeros and a log-sum-exp of minus infinity are for queries that see nothing.)"""
+"""A score that is no number shows in what it reaches, and nowhere else: the query's output and log-sum-exp, and from there the weights of
+the slots that it sees.  (Zeros and a log-sum-exp of minus infinity are for queries that see nothing.)"""
 import math
 
 import pytest
@@ -7,7 +8,7 @@ import torch
 import paper_2509_15763_b200 as ug
 
 from chunk_routes import ROUTES, cache_of, launched
-from chunk_util import DEV, PG, Cache, attn_ref, attn_workspace, check_attn, cu_of
+from chunk_util import DEV, PG, Cache, attn_ref, attn_workspace, check_attn, cu_of, weigh_ref
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
@@ -93,3 +94,29 @@ def test_keys_that_are_none_in_walks_that_are_cut(dim):
             bad[-1, 0] = True
             cache = Cache([L], hkv, dim, seed=slot)
             check(*attend(cache, q, rows), ref, bad, f"{rows} all")
+
+
+@pytest.mark.parametrize("rows,lens,hq,hkv", [([1, 1], [300, 700], 8, 2), ([8, 4], [300, 700], 32, 1), ([100, 90], [400, 700], 8, 2), ([200, 64], [900, 64], 12, 4), ([40], [300], 7, 1)])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_weights_of_queries_that_are_none(rows, lens, hq, hkv, dim):
+    """Each query in turn: the slots that it sees get no number, in its head's KV head; all others theirs."""
+    cache, n, G = Cache(lens, hkv, dim, seed=hq), sum(rows), hq // hkv
+    q = queries(n, hq, dim)
+    lse = attn_ref(cache, q, rows, dim ** -0.5)[1].float()
+    for i in sorted({0, 1 % n, 2 % n, n // 2, n // 2 + 5 if n > 12 else 0, n - 1}):
+        head = (3 * i + 1) % hq
+        q2, lse2 = q.clone(), lse.clone()
+        q2[i, head], lse2[i, head] = NAN, NAN
+        d = cache.device()
+        out = torch.full_like(d["w"], 5.0)
+        ug.unigist_cache_weigh(q2.to(DEV), cu_of(rows).to(DEV), lse2.to(DEV), d["k"], d["table"], d["lens"], d["w"], out)
+        ug.unigist_device_status()
+        b = 0 if i < rows[0] else 1
+        seen = lens[b] - rows[b] + (i - (0 if b == 0 else rows[0]))   # the last slot that it sees
+        for c, want in weigh_ref(cache, q, rows, lse, dim ** -0.5, 1.0, cache.w).items():
+            got = cache.rows(out, c)
+            none = torch.zeros_like(got, dtype=torch.bool)
+            if c == b:
+                none[head // G, : seen + 1] = True
+            assert torch.isnan(got[none]).all(), f"query {i} of {rows}: a weight hides it"
+            assert (((got - want).abs() - 1e-4 * want)[~none] <= 1e-30).all(), (i, c)   # (the bound of the tests of that call)
