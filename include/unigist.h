@@ -330,6 +330,7 @@ int32_t unigist_decode(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_hea
  *    table's room; nothing outside the buffers is read or written whatever they say (a page outside the cache is never
  *    written; what is read for it is some page of the cache).  A page that a call writes belongs to one sequence and
  *    stands once in its row of the table.
+ *  - bf16 tensors (and the weights of unigist_cache_evict) are 16-byte aligned, all other fp32 and int32 ones 4-byte.
  *  - num_rows may be 0.  All calls can be captured into a graph; two calls that may overlap need workspaces of their own.
  */
 

@@ -55,6 +55,13 @@ size_t rows_bytes(int64_t stride, int32_t rows, int32_t heads, int32_t D) {
   return rows > 0 ? ((size_t)(rows - 1) * (size_t)stride + (size_t)heads * D) * 2 : 0;
 }
 
+// Whether all of some 32-bit numbers' addresses (which may be null) are aligned.
+template <typename... P>
+bool aligned4(P... p) {
+  return (((reinterpret_cast<uintptr_t>(p) & 3) == 0) && ...);
+}
+int32_t misaligned4() { return fail(UNIGIST_ERR_ALIGNMENT, "32-bit numbers must be 4-byte aligned"); }
+
 bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
   const char *x = (const char*)a, *y = (const char*)b;
   return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
@@ -71,6 +78,7 @@ int32_t check_scale(float softmax_scale, int32_t D, float* scale) {
 
 int32_t check_rope(int32_t D, const int32_t* pos_ids, int32_t num_axes, const uint8_t* freq_axis, float theta_base) {
   if (!pos_ids || !freq_axis) return fail(UNIGIST_ERR_INVALID_ARG, "a pointer is NULL");
+  if (!aligned4(pos_ids)) return misaligned4();
   if (num_axes < 1 || num_axes > 255) return fail(UNIGIST_ERR_INVALID_ARG, "num_axes %d is not in 1 .. 255", num_axes);
   if (!(theta_base > 1.f) || std::isinf(theta_base)) return fail(UNIGIST_ERR_INVALID_ARG, "theta_base must be finite and above 1");
   for (int j = 0; j < D / 2; ++j)
@@ -88,7 +96,8 @@ int32_t unigist_rope_axes(int32_t num_tokens, int32_t heads, int32_t head_dim, c
   if (int32_t rc = check_num_rows(num_tokens)) return rc;
   if (int32_t rc = check_heads(heads, head_dim)) return rc;
   if (flags & ~UNIGIST_ROPE_INVERSE) return fail(UNIGIST_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
-  if (int32_t rc = check_rope(head_dim, num_tokens ? pos_ids : (const int32_t*)freq_axis, num_axes, freq_axis, theta_base)) return rc;
+  static const int32_t no_positions = 0;
+  if (int32_t rc = check_rope(head_dim, num_tokens ? pos_ids : &no_positions, num_axes, freq_axis, theta_base)) return rc;
   if (num_tokens == 0) return UNIGIST_OK;
   if (int32_t rc = check_rows(src, src_stride, num_tokens, heads, head_dim)) return rc;
   if (int32_t rc = check_rows(dst, dst_stride, num_tokens, heads, head_dim)) return rc;
@@ -110,6 +119,7 @@ int32_t unigist_chunk_append(int32_t S, int32_t Hkv, int32_t D, int32_t num_rows
   if (int32_t rc = check_num_rows(num_rows)) return rc;
   if (!cu_rows || !kc || !vc || !table || !seq_lens || !new_lens) return fail(UNIGIST_ERR_INVALID_ARG, "a pointer is NULL");
   if (!aligned16(kc) || !aligned16(vc)) return fail(UNIGIST_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!aligned4(cu_rows, table, seq_lens, new_lens, weights)) return misaligned4();
   if (overlap(seq_lens, (size_t)S * 4, new_lens, (size_t)S * 4)) return fail(UNIGIST_ERR_INVALID_ARG, "new_lens overlaps seq_lens");
   if (num_rows > 0) {
     if (int32_t rc = check_rows(k_new, k_stride, num_rows, Hkv, D)) return rc;
@@ -144,6 +154,7 @@ int32_t unigist_chunk_attn(int32_t S, int32_t Hq, int32_t Hkv, int32_t D, float 
   if (int32_t rc = check_rows(q, q_stride, num_rows, Hq, D)) return rc;
   if (!aligned16(kc) || !aligned16(vc) || !aligned16(o) || !aligned16(workspace))
     return fail(UNIGIST_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!aligned4(cu_rows, table, seq_lens, lse)) return misaligned4();
   if (overlap(q, rows_bytes(q_stride, num_rows, Hq, D), o, rows_bytes((int64_t)Hq * D, num_rows, Hq, D)))
     return fail(UNIGIST_ERR_INVALID_ARG, "o overlaps q");
   const size_t need = chunk_attn_scratch_bytes(S, num_rows, Hq, Hkv, D, max_blocks);
@@ -166,6 +177,7 @@ int32_t unigist_cache_weigh(int32_t S, int32_t Hq, int32_t Hkv, int32_t D, float
   if (!cu_rows || !kc || !table || !seq_lens || !weights_out || (decay > 0.f && !weights_in))
     return fail(UNIGIST_ERR_INVALID_ARG, "a pointer is NULL");
   if (!aligned16(kc)) return fail(UNIGIST_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!aligned4(cu_rows, lse, table, seq_lens, weights_in, weights_out)) return misaligned4();
   if (num_rows > 0) {
     if (!lse) return fail(UNIGIST_ERR_INVALID_ARG, "a pointer is NULL");
     if (int32_t rc = check_rows(q, q_stride, num_rows, Hq, D)) return rc;
@@ -189,6 +201,7 @@ int32_t unigist_cache_evict(int32_t S, int32_t Hkv, int32_t D, int32_t keep, int
   if (!kc || !vc || !weights || !table || !seq_lens || !new_table || !new_lens || !kept_idx)
     return fail(UNIGIST_ERR_INVALID_ARG, "a pointer is NULL");
   if (!aligned16(kc) || !aligned16(vc) || !aligned16(weights)) return fail(UNIGIST_ERR_ALIGNMENT, "tensor pointers must be 16-byte aligned");
+  if (!aligned4(table, seq_lens, new_table, new_lens, kept_idx)) return misaligned4();
   if (overlap(seq_lens, (size_t)S * 4, new_lens, (size_t)S * 4)) return fail(UNIGIST_ERR_INVALID_ARG, "new_lens overlaps seq_lens");
   const int64_t most = (int64_t)max_blocks * UNIGIST_PAGE_TOKENS < keep ? (int64_t)max_blocks * UNIGIST_PAGE_TOKENS : keep;
   if (new_max_blocks < 1 || (int64_t)new_max_blocks * UNIGIST_PAGE_TOKENS < most)
