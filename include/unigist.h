@@ -365,8 +365,8 @@ int32_t unigist_chunk_append(int32_t num_seqs, int32_t num_kv_heads, int32_t hea
  * sees slots 0 .. L - n + i.  o [num_rows, Hq, D] device bf16, lse [num_rows, Hq] device fp32 (natural log, nullable).  A query
  * that sees nothing (L - n + i < 0) gets O = 0 and LSE = -inf; one with a score that is NaN or infinite, NaN in both.  What lies in the pages behind slot L - 1 does not
  * matter, whatever it is (unigist_decode wants numbers there); a value that is not finite reaches the queries of its 128-slot tile that come before it as well.
- * workspace: unigist_chunk_attn_workspace_bytes bytes, 16-byte aligned; nothing in it has to start at zero.  o overlaps none
- * of the inputs.  The results are the same bit for bit from run to run; they depend on the whole batch in their last bits.
+ * workspace: unigist_chunk_attn_workspace_bytes bytes, 16-byte aligned; nothing in it has to start at zero.  o and
+ * lse overlap none of the inputs, nor each other or the workspace.  The results are the same bit for bit from run to run; they depend on the whole batch in their last bits.
  */
 size_t unigist_chunk_attn_workspace_bytes(int32_t num_seqs, int32_t num_rows, int32_t num_q_heads, int32_t num_kv_heads,
                                           int32_t head_dim, int32_t max_blocks_per_seq);

@@ -160,6 +160,17 @@ int32_t unigist_chunk_attn(int32_t S, int32_t Hq, int32_t Hkv, int32_t D, float 
   const size_t need = chunk_attn_scratch_bytes(S, num_rows, Hq, Hkv, D, max_blocks);
   if (!workspace || ws_bytes < need)
     return fail(UNIGIST_ERR_WORKSPACE, "chunk attention needs %zu bytes of workspace, got %zu", need, ws_bytes);
+  const size_t o_bytes = rows_bytes((int64_t)Hq * D, num_rows, Hq, D), lse_bytes = lse ? (size_t)num_rows * Hq * 4 : 0;
+  const size_t cache_bytes = (size_t)num_blocks * Hkv * UNIGIST_PAGE_TOKENS * D * 2;
+  const struct {
+    const void* p;
+    size_t bytes;
+  } others[] = {{kc, cache_bytes}, {vc, cache_bytes}, {cu_rows, ((size_t)S + 1) * 4}, {table, (size_t)S * max_blocks * 4}, {seq_lens, (size_t)S * 4}, {workspace, need}};
+  for (const auto& x : others)
+    if (overlap(o, o_bytes, x.p, x.bytes) || overlap(lse, lse_bytes, x.p, x.bytes))
+      return fail(UNIGIST_ERR_INVALID_ARG, "o or lse overlaps an input or the workspace");
+  if (overlap(o, o_bytes, lse, lse_bytes) || overlap(lse, lse_bytes, q, rows_bytes(q_stride, num_rows, Hq, D)))
+    return fail(UNIGIST_ERR_INVALID_ARG, "lse overlaps o or q");
   const ChunkBatch b = {cu_rows, seq_lens, table, S, num_rows, max_blocks, num_blocks};
   return launch_chunk_attn(b, Hq, Hkv, D, scale, q, q_stride, kc, vc, o, lse, workspace, (cudaStream_t)stream);
 }

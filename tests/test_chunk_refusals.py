@@ -71,3 +71,22 @@ def evict(**kw):
 def test_numbers_that_are_not_aligned(call, name, off):
     """A 32-bit number at an odd address is a fault on the device."""
     refused(lambda: call(**{name: at(30) + off}), ALIGN)
+
+
+# (S 2, Hq 4, Hkv 2, D 64, 3 rows, 4 pages of 64: what each argument spans)
+O_BYTES, CACHE, SMALL = 3 * 4 * 64 * 2, 4 * 2 * 64 * 64 * 2, 8
+
+
+@pytest.mark.parametrize("name,bytes_", [("q", (2 * 256 + 4 * 64) * 2), ("cu", 12), ("kc", CACHE), ("vc", CACHE), ("table", 16), ("lens", 8), ("lse", 3 * 4 * 4)])
+@pytest.mark.parametrize("where", ["start", "end", "inside"])
+def test_an_output_of_the_attention_over_one_of_its_inputs(name, bytes_, where):
+    place = at(30)
+    o = {"start": place + (bytes_ - 1) // 16 * 16, "end": place - O_BYTES + 16, "inside": place}[where]
+    refused(lambda: attn(**{name: place, "o": o}), INVALID)
+
+
+def test_an_output_of_the_attention_over_its_workspace():
+    need = ug.unigist_chunk_attn_workspace_bytes(2, 3, 4, 2, 64, 2)
+    refused(lambda: attn(ws=at(30), o=at(30) + need - 16, ws_bytes=need), INVALID)
+    refused(lambda: attn(ws=at(30), o=at(30) - O_BYTES + 16, ws_bytes=need), INVALID)
+    refused(lambda: attn(ws=at(30), lse=at(30) + need - 16, ws_bytes=need), INVALID)
