@@ -46,19 +46,28 @@ struct Args {
     if (at >= n) raise(PyExc_TypeError, "too few arguments");
     return a[at++];
   }
-  Arg tensor() {  // (data_ptr() throws for a tensor without storage: a transform's or a tracer's)
+  const at::Tensor* contiguous() {  // null for None
     PyObject* o = next();
-    if (o == Py_None) return {nullptr, nullptr, 0};
+    if (o == Py_None) return nullptr;
     if (!THPVariable_Check(o)) raise(PyExc_TypeError, "expected a torch.Tensor");
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_cuda() || !t.is_contiguous()) raise(PyExc_ValueError, "tensors must be contiguous CUDA tensors");
-    return {&t, t.data_ptr(), (size_t)t.numel() * t.element_size()};
+    return &t;
   }
-  // The calls on chunks say what they take: the element type, on the current device.
+  static Arg arg(const at::Tensor* t) {  // (data_ptr() throws for a tensor without storage: a transform's or a tracer's)
+    return t ? Arg{t, t->data_ptr(), (size_t)t->numel() * t->element_size()} : Arg{nullptr, nullptr, 0};
+  }
+  Arg tensor() { return arg(contiguous()); }
+  // The calls on chunks say what they take: on the current device, of an element type (a workspace of any).
   Arg tensor(at::ScalarType type, const char* name) {
-    const Arg x = tensor();
-    if (x.t) check(*x.t, type, name);
-    return x;
+    const at::Tensor* t = contiguous();
+    if (t) check(*t, type, name);
+    return arg(t);
+  }
+  Arg workspace() {
+    const at::Tensor* t = contiguous();
+    if (t) check_device(*t, "workspace");
+    return arg(t);
   }
   // A [rows, heads, head_dim] tensor whose heads lie together; the rows may be any distance apart (part of a projection's output).
   Arg rows(const char* name, int64_t* stride) {
@@ -77,6 +86,9 @@ struct Args {
   }
   static void check(const at::Tensor& t, at::ScalarType type, const char* name) {
     if (t.scalar_type() != type) raise(PyExc_ValueError, (std::string(name) + " must be " + c10::toString(type)).c_str());
+    check_device(t, name);
+  }
+  static void check_device(const at::Tensor& t, const char* name) {
     if (t.device().index() != c10::cuda::current_device()) raise(PyExc_ValueError, (std::string(name) + " is not on the current device").c_str());
   }
   std::vector<uint8_t> byte_list(const char* what) {
@@ -401,7 +413,7 @@ int32_t chunk_attn(Args& a) {
   const Arg kc = a.tensor(at::kBFloat16, "k_cache"), vc = a.tensor(at::kBFloat16, "v_cache");
   b.table = a.tensor(at::kInt, "block_table");
   b.lens = a.tensor(at::kInt, "seq_lens");
-  const Arg o = a.tensor(at::kBFloat16, "o"), lse = a.tensor(at::kFloat, "lse"), ws = a.tensor();
+  const Arg o = a.tensor(at::kBFloat16, "o"), lse = a.tensor(at::kFloat, "lse"), ws = a.workspace();
   const float scale = (float)a.real();
   void* st = a.stream();
   b.expect_fits();
