@@ -26,7 +26,9 @@
 // with the TMA producer warp and the MMA issuer / TMEM owner warp, which hands most of its registers
 // to the softmax warpgroups.  TMEM: S0 | S1 | O0 | O1, 128 columns each.
 #include <algorithm>
+#include <atomic>
 
+#include "chunk_tma.cuh"
 #include "softmax_row.cuh"
 #include "ug_common.cuh"
 
@@ -540,7 +542,8 @@ typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void
                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 int32_t get_encode_fn(EncodeFn* out) {
-  static EncodeFn encode = nullptr;
+  static std::atomic<EncodeFn> found{nullptr};  // (calls may come from several threads; they all find the same)
+  EncodeFn encode = found.load(std::memory_order_relaxed);
   if (!encode) {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
@@ -548,6 +551,7 @@ int32_t get_encode_fn(EncodeFn* out) {
     if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
       return fail(UNIGIST_ERR_CUDA, "cuTensorMapEncodeTiled is not available: %s", cudaGetErrorString(e));
     encode = reinterpret_cast<EncodeFn>(fn);
+    found.store(encode, std::memory_order_relaxed);
   }
   *out = encode;
   return UNIGIST_OK;
@@ -641,6 +645,21 @@ int32_t encode_map_2d_bf16(CUtensorMap* map, const void* base, long long rows, i
   const cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   const cuuint32_t estr[2] = {1, 1};
   CUresult r = encode_bound(encode, map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(UNIGIST_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
+  return UNIGIST_OK;
+}
+
+int32_t encode_row_map(CUtensorMap* map, const void* base, int D, int heads, long long rows, int64_t stride, int box_heads,
+                       int box_rows) {
+  EncodeFn encode;
+  if (int32_t rc = get_encode_fn(&encode)) return rc;
+  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = encode_bound(encode, map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(UNIGIST_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);

@@ -780,36 +780,6 @@ int32_t launch_chunk_combine(const ChunkParams& P, int D, int grid, cudaStream_t
   return check_launch("chunk combine kernel");
 }
 
-int32_t encode_row_map(CUtensorMap* map, const void* base, int D, int heads, long long rows, int64_t stride, int box_heads,
-                       int box_rows) {
-  typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                               const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  void* fn = nullptr;
-  cudaDriverEntryPointQueryResult found;
-  static EncodeFn encode = nullptr;
-  if (!encode) {
-    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
-    if (e != cudaSuccess || found != cudaDriverEntryPointSuccess || !fn)
-      return fail(UNIGIST_ERR_CUDA, "cuTensorMapEncodeTiled is not available: %s", cudaGetErrorString(e));
-    encode = reinterpret_cast<EncodeFn>(fn);
-  }
-  const cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)heads, (cuuint64_t)rows};
-  const cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, estr[3] = {1, 1, 1};
-  auto call = [&] {
-    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  };
-  CUresult r = call();
-  int dev = 0;
-  // (a thread whose first CUDA call this is has no context yet; setting the device it would use makes it current)
-  if (r == CUDA_ERROR_INVALID_CONTEXT && cudaGetDevice(&dev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess) r = call();
-  if (r != CUDA_SUCCESS) return fail(UNIGIST_ERR_CUDA, "cuTensorMapEncodeTiled failed with code %d", (int)r);
-  return UNIGIST_OK;
-}
-
 size_t chunk_attn_scratch_bytes(int S, int num_rows, int Hq, int Hkv, int D, int max_blocks) {
   if (num_rows < 1) return 0;
   const int G = Hq / Hkv;
