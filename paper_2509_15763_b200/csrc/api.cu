@@ -98,6 +98,21 @@ int32_t check_launch(const char* what) {
   return UNIGIST_OK;
 }
 
+namespace {
+// The flags of all kernels with bounded waits, taken (and put back to zero) by one launch and one copy: a copy for each
+// took 100 us a call, this 20.
+constexpr int kFlags = 8;
+struct TimeoutFlags {
+  unsigned int* at[kFlags];
+};
+__device__ unsigned int g_timed_out;
+__global__ void take_timeouts_kernel(TimeoutFlags flags) {
+  const bool mine = threadIdx.x < kFlags && atomicExch(flags.at[threadIdx.x], 0u) != 0;
+  const bool any = __any_sync(0xffffffffu, mine);
+  if (threadIdx.x == 0) g_timed_out = any;
+}
+}  // namespace
+
 constexpr int kMaxGridYZ = 65535;
 
 int32_t check_problem(const unigist_problem* p, Geom* g, float* scale) {
@@ -299,18 +314,17 @@ int32_t unigist_attn_fwd(const unigist_problem* p, const void* q, const void* k,
 int32_t unigist_device_status(void) {
   cudaError_t e = cudaDeviceSynchronize();
   if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "cudaDeviceSynchronize: %s", cudaGetErrorString(e));
-  bool timed_out = false;
-  bool bwd_timed_out = false;
-  if (int32_t rc = fwd_sm100_take_timeout(&timed_out)) return rc;
-  if (int32_t rc = bwd_sm100_take_timeout(&bwd_timed_out)) return rc;
-  bool dec_timed_out = false;
-  if (int32_t rc = decode_take_timeout(&dec_timed_out)) return rc;
-  bool self_timed_out = false;
-  if (int32_t rc = selftest_take_timeout(&self_timed_out)) return rc;
-  bool chunk_timed_out = false, weigh_timed_out = false;
-  if (int32_t rc = chunk_attn_take_timeout(&chunk_timed_out)) return rc;
-  if (int32_t rc = cache_weigh_take_timeout(&weigh_timed_out)) return rc;
-  if (timed_out || bwd_timed_out || dec_timed_out || self_timed_out || chunk_timed_out || weigh_timed_out) return fail(UNIGIST_ERR_TIMEOUT, "a kernel gave up on a bounded wait; its outputs are invalid");
+  int32_t (*const flag_of[kFlags])(unsigned int**) = {fwd_sm100_timeout_flag,  bwd_sm100_timeout_flag, decode_timeout_flag,     selftest_timeout_flag,
+                                                      chunk_attn_timeout_flag, chunk_few_timeout_flag, chunk_thin_timeout_flag, cache_weigh_timeout_flag};
+  TimeoutFlags flags;
+  for (int i = 0; i < kFlags; ++i)
+    if (int32_t rc = flag_of[i](&flags.at[i])) return rc;
+  take_timeouts_kernel<<<1, 32>>>(flags);
+  if (int32_t rc = check_launch("device status kernel")) return rc;
+  unsigned int timed_out = 0;
+  e = cudaMemcpyFromSymbol(&timed_out, g_timed_out, sizeof(timed_out));
+  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
+  if (timed_out) return fail(UNIGIST_ERR_TIMEOUT, "a kernel gave up on a bounded wait; its outputs are invalid");
   return UNIGIST_OK;
 }
 

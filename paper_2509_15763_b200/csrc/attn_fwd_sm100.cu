@@ -785,13 +785,6 @@ int32_t launch_fwd_sm100_runs(const SeqRun* runs, int n_runs, const unigist_prob
   return UNIGIST_OK;
 }
 
-int32_t fwd_sm100_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_fwd_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_fwd_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t fwd_sm100_timeout_flag(unsigned int** at) { return flag_address(at, g_fwd_timeout); }
 
 }  // namespace ug

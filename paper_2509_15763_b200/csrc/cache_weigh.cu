@@ -465,13 +465,6 @@ int32_t launch_cache_weigh(const ChunkBatch& b, int Hq, int Hkv, int D, float sc
   return D == 128 ? go<128, 128>(mq, mk, P, grid, st) : go<64, 128>(mq, mk, P, grid, st);
 }
 
-int32_t cache_weigh_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_weigh_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_weigh_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t cache_weigh_timeout_flag(unsigned int** at) { return flag_address(at, g_weigh_timeout); }
 
 }  // namespace ug

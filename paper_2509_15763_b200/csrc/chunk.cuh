@@ -78,11 +78,13 @@ int32_t launch_chunk_append(const ChunkBatch& b, int Hkv, int D, const void* k_n
 size_t chunk_attn_scratch_bytes(int S, int num_rows, int Hq, int Hkv, int D, int max_blocks);
 int32_t launch_chunk_attn(const ChunkBatch& b, int Hq, int Hkv, int D, float scale, const void* q, int64_t q_stride,
                           const void* kc, const void* vc, void* o, float* lse, void* ws, cudaStream_t st);
-int32_t chunk_attn_take_timeout(bool* timed_out);
+int32_t chunk_attn_timeout_flag(unsigned int** at);
+int32_t chunk_few_timeout_flag(unsigned int** at);
+int32_t chunk_thin_timeout_flag(unsigned int** at);
 int32_t launch_cache_weigh(const ChunkBatch& b, int Hq, int Hkv, int D, float scale, const void* q, int64_t q_stride,
                            const float* lse, const void* kc, const float* weights_in, float decay, float* weights_out,
                            cudaStream_t st);
-int32_t cache_weigh_take_timeout(bool* timed_out);
+int32_t cache_weigh_timeout_flag(unsigned int** at);
 int32_t launch_cache_evict(const ChunkBatch& b, int Hkv, int D, int keep, int keep_first, int keep_last, void* kc, void* vc,
                            float* weights, const int32_t* new_table, int new_max_blocks, int32_t* new_lens, int32_t* kept_idx,
                            cudaStream_t st);

@@ -814,17 +814,6 @@ int32_t launch_chunk_attn(const ChunkBatch& b, int Hq, int Hkv, int D, float sca
   return D == 128 ? go<128>(mq, mk, mv, P, grid, st) : go<64>(mq, mk, mv, P, grid, st);
 }
 
-int32_t chunk_attn_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_chunk_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_chunk_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  bool few = false, thin = false;
-  if (int32_t rc = chunk_few_take_timeout(&few)) return rc;
-  if (int32_t rc = chunk_thin_take_timeout(&thin)) return rc;
-  *timed_out = *timed_out || few || thin;
-  return UNIGIST_OK;
-}
+int32_t chunk_attn_timeout_flag(unsigned int** at) { return flag_address(at, g_chunk_timeout); }
 
 }  // namespace ug

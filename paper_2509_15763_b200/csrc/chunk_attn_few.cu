@@ -481,13 +481,6 @@ int32_t launch_chunk_few(ChunkParams P, int D, const CUtensorMap& mk, const CUte
   return D == 128 ? go<128, 2>(P, plan, mk, mv, st) : go<64, 2>(P, plan, mk, mv, st);
 }
 
-int32_t chunk_few_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_few_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_few_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t chunk_few_timeout_flag(unsigned int** at) { return flag_address(at, g_few_timeout); }
 
 }  // namespace ug

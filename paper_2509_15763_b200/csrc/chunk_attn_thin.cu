@@ -407,13 +407,6 @@ int32_t launch_chunk_thin(ChunkParams P, const void* q, int64_t q_stride, const 
   return launch_chunk_combine(P, D, grid, st);
 }
 
-int32_t chunk_thin_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_thin_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_thin_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t chunk_thin_timeout_flag(unsigned int** at) { return flag_address(at, g_thin_timeout); }
 
 }  // namespace ug

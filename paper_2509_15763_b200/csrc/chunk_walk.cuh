@@ -192,11 +192,9 @@ enum { kChunkRows, kChunkFew, kChunkThin };
 int chunk_route(int S, int num_rows, int G, int Hkv, int D, int max_blocks);
 size_t chunk_few_scratch_bytes(int S, int num_rows, int Hq, int Hkv, int D, int max_blocks);
 int32_t launch_chunk_few(ChunkParams P, int D, const CUtensorMap& mk, const CUtensorMap& mv, void* ws, cudaStream_t st);
-int32_t chunk_few_take_timeout(bool* timed_out);
 inline int chunk_thin_grid() { return sm_count() < 256 ? sm_count() : 256; }
 size_t chunk_thin_scratch_bytes();
 int32_t launch_chunk_thin(ChunkParams P, const void* q, int64_t q_stride, const CUtensorMap& mk, const CUtensorMap& mv, void* ws, cudaStream_t st);
-int32_t chunk_thin_take_timeout(bool* timed_out);
 
 // Bytes of `grid` shares' parts, and the pointers to them.
 inline size_t chunk_parts_bytes(int grid, int rows, int D) {

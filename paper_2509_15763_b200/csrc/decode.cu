@@ -750,14 +750,7 @@ int32_t launch_decode(int S, int Hq, int Hkv, int D, float scale, const void* q,
   return check_launch("decode combine kernel");
 }
 
-int32_t decode_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_decode_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_decode_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t decode_timeout_flag(unsigned int** at) { return flag_address(at, g_decode_timeout); }
 
 }  // namespace ug
 

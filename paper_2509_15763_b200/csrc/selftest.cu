@@ -46,13 +46,6 @@ int32_t launch_selftest_wait(cudaStream_t st) {
   return check_launch("bounded-wait self-check kernel");
 }
 
-int32_t selftest_take_timeout(bool* timed_out) {
-  unsigned int flag = 0, zero = 0;
-  cudaError_t e = cudaMemcpyFromSymbol(&flag, g_selftest_timeout, sizeof(flag));
-  if (e == cudaSuccess && flag) e = cudaMemcpyToSymbol(g_selftest_timeout, &zero, sizeof(zero));
-  if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
-  *timed_out = flag != 0;
-  return UNIGIST_OK;
-}
+int32_t selftest_timeout_flag(unsigned int** at) { return flag_address(at, g_selftest_timeout); }
 
 }  // namespace ug

@@ -192,6 +192,13 @@ void launch_chained(void (*kern)(KArgs...), dim3 grid, int threads, size_t smem,
 }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// Where a file's flag "a kernel gave up on a bounded wait" lies on the current device; the launchers' files name theirs below.
+template <typename Symbol>
+int32_t flag_address(unsigned int** at, const Symbol& symbol) {
+  const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void**>(at), symbol);
+  return e == cudaSuccess ? UNIGIST_OK : fail(UNIGIST_ERR_CUDA, "reading the device status: %s", cudaGetErrorString(e));
+}
+
 // Kernel launchers (one per .cu file).
 int32_t launch_layout(const Geom& g, int32_t* sp, int32_t* up, int32_t* pos, cudaStream_t st);
 int32_t launch_rope(const Geom& g, int B, int heads, int D, float theta_base, bool to_shifted, bool from_shifted,
@@ -219,7 +226,7 @@ struct SeqRun {
 };
 int32_t launch_fwd_sm100_runs(const SeqRun* runs, int n_runs, const unigist_problem& p, float scale, const void* q,
                               const void* k, const void* v, void* o, float* lse, cudaStream_t st);
-int32_t fwd_sm100_take_timeout(bool* timed_out);
+int32_t fwd_sm100_timeout_flag(unsigned int** at);
 int32_t launch_bwd_sm100(const Geom& g, const unigist_problem& p, float scale, const void* q,
                          const void* k, const void* v, const void* o, const float* lse,
                          const void* d_o, void* dq, void* dk, void* dv, void* workspace, bool spread,
@@ -237,7 +244,7 @@ size_t bwd_scratch_bytes(long long tokens, int Hq, int D, bool dout_fp32, bool f
 // queries is cut into chunks (0 where nothing is cut), for the units of ONE launch of the fused backward.  in_turn: one problem,
 // not a packed sample.  spread: walks that are cut only to spread them over idle SMs too; without them, the least that is accepted.
 size_t bwd_partial_bytes(const SeqRun* runs, int n_runs, int Hq, int Hkv, bool in_turn, bool spread);
-int32_t bwd_sm100_take_timeout(bool* timed_out);
+int32_t bwd_sm100_timeout_flag(unsigned int** at);
 int32_t launch_compact_gather(const Geom& g, const unigist_problem& p, const void* k,
                               const void* v, void* kc, void* vc, int num_blocks,
                               const int32_t* table, int max_blocks, int32_t* seq_lens,
@@ -261,8 +268,8 @@ int32_t launch_cache_append(const Geom& g, const unigist_problem& p, int is_gist
 // Decode scratch: what the plan of a call uses at its best, and the least that is accepted.
 size_t decode_scratch_bytes(int S, int Hq, int Hkv, int D, int max_blocks);
 size_t decode_min_scratch_bytes(int S, int Hq, int Hkv, int D, int max_blocks);
-int32_t decode_take_timeout(bool* timed_out);
+int32_t decode_timeout_flag(unsigned int** at);
 int32_t launch_selftest_wait(cudaStream_t st);
-int32_t selftest_take_timeout(bool* timed_out);
+int32_t selftest_timeout_flag(unsigned int** at);
 
 }  // namespace ug
