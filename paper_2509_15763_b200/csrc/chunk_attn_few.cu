@@ -445,7 +445,12 @@ FewPlan few_plan(int S, int num_rows, int G, int Hkv, int max_blocks) {
 template <int D, int MT>
 int32_t go(const ChunkParams& P, const FewPlan& plan, const CUtensorMap& mk, const CUtensorMap& mv, cudaStream_t st) {
   using F = Few<D, MT>;
-  const auto kern = plan.c ? chunk_few_kernel<D, MT, false> : chunk_few_kernel<D, MT, true>;
+  auto kern = chunk_few_kernel<D, MT, false>;
+  if constexpr (D == 64) {  // (the calls of heads of 128 that are dealt out go to the kernel with the operands turned round)
+    if (!plan.c) kern = chunk_few_kernel<D, MT, true>;
+  } else if (!plan.c) {
+    return fail(UNIGIST_ERR_UNSUPPORTED, "no kernel for this cut");
+  }
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
   if (e == cudaSuccess && plan.c > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e != cudaSuccess) return fail(UNIGIST_ERR_CUDA, "cudaFuncSetAttribute: %s", cudaGetErrorString(e));
