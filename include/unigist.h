@@ -311,11 +311,16 @@ int32_t unigist_decode(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_hea
 
 /*
  * Ragged chunks of new tokens over a paged cache.  The calls below serve what the token-by-token loop above does not: several
- * new tokens of a sequence at once (drafted tokens to be verified, a part of a prompt) over whatever the cache holds, in one
+ * new tokens of a sequence at once (drafted tokens to be verified, a part of a prompt) over all slots below its length, in one
  * batch with sequences that bring other numbers of tokens, and caches whose slots are no positions because some were evicted.
  * Together: unigist_rope_axes (queries), unigist_chunk_append (keys, rotated on the way, and values), unigist_chunk_attn,
  * unigist_cache_weigh, unigist_cache_evict; unigist_decode reads the same caches.  (The paper has no counterpart: its cache
  * keeps every gist.  Slots of a gist cache are evicted like any others; not while a unigist_cache_append state refers to them.)
+ * They know nothing of that state.  From the first raw token of a unit to the one before its last, a cache that unigist_cache_append
+ * maintains has freed slots below its length: unigist_decode_step leaves them out, unigist_chunk_attn and unigist_cache_weigh would
+ * attend to them; unigist_chunk_append does not advance the state.  So over such a cache they serve whole units only (as
+ * unigist_kv_compact and unigist_prefill_chunk leave it, or unigist_cache_append after a unit's last raw token or its gist), for
+ * tokens that are dropped again or that open no unit.
  *
  * Conventions of these calls
  *  - num_rows rows of all sequences lie one after the other: rows [cu_rows[b], cu_rows[b + 1]) are the chunk of sequence b
@@ -363,8 +368,12 @@ int32_t unigist_chunk_append(int32_t num_seqs, int32_t num_kv_heads, int32_t hea
 /*
  * Attention of the chunks over the cache: query i of the n of sequence b, whose length seq_lens[b] = L includes the chunk,
  * sees slots 0 .. L - n + i.  o [num_rows, Hq, D] device bf16, lse [num_rows, Hq] device fp32 (natural log, nullable).  A query
- * that sees nothing (L - n + i < 0) gets O = 0 and LSE = -inf; one with a score that is NaN or infinite, NaN in both.  What lies in the pages behind slot L - 1 does not
- * matter, whatever it is (unigist_decode wants numbers there); a value that is not finite reaches the queries of its 128-slot tile that come before it as well.
+ * that sees nothing (L - n + i < 0, or scores of -inf alone) gets O = 0 and LSE = -inf; one with a score that is NaN or +inf,
+ * NaN in both.  What lies in the pages behind slot L - 1 does not
+ * matter, whatever it is (unigist_decode wants numbers there); a value that is not finite, or beyond 1e30, reaches the queries of its
+ * 128-slot tile that come before it as well.  Scores, maxima and sums are fp32; as in unigist_attn_fwd the weights go into the
+ * product with V as bf16 (2^-8 of the sum of their products' sizes), and with chunks of many rows a quarter of the exponentials is a
+ * polynomial that is off by 7.5e-5, in O and LSE alike.
  * workspace: unigist_chunk_attn_workspace_bytes bytes, 16-byte aligned; nothing in it has to start at zero.  o and
  * lse overlap none of the inputs, nor each other or the workspace.  The results are the same bit for bit from run to run; they depend on the whole batch in their last bits.
  */
@@ -381,7 +390,8 @@ int32_t unigist_chunk_attn(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv
  *                    of exp(scale * q_i . k_j - lse_i).
  * lse [num_rows, Hq]: what unigist_chunk_attn (or, for one row per sequence, unigist_decode) returned for the same queries
  * over the same cache.  decay in [0, 1]; with 0 weights_in is not read and may be NULL.  weights_out may be weights_in; the
- * weights of all other slots are left as they were.  Same bits from run to run.
+ * weights of all other slots are left as they were.  A slot's weights are added up in fp32, in an order that goes by the sizes
+ * alone: the same bits from run to run.
  */
 int32_t unigist_cache_weigh(int32_t num_seqs, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float softmax_scale,
                             int32_t num_rows, const void* q, int64_t q_stride, const int32_t* cu_rows, const float* lse,

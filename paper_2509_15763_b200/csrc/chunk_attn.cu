@@ -121,6 +121,8 @@ __device__ __forceinline__ float half_exp(const uint32_t (&sc)[kHalf], uint32_t 
 
 // kWaves: one sequence of at least as many units as there are blocks (a kernel of its own: what the others carry along for it in
 // their registers made a mixed batch 3 - 8 % longer).
+// All of them spill (ptxas, bytes stored / loaded: heads of 64 168 / 240, with kWaves 324 / 444; heads of 128 284 / 344 and 460 / 616):
+// it goes by the registers that a thread has at the launch, 96 and 168, whatever its role has later.
 template <int D, bool kWaves>
 __global__ void __launch_bounds__(ChunkShape<D>::kThreads, 1)
 chunk_attn_sm100_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,

@@ -54,6 +54,7 @@ struct Few {
   static_assert((kThreads + 1 + kThreads / 32 + 1) * 8 <= kQBytes && kRows * D * 2 <= kQBytes && kRows * D * 4 <= kStage && D / 8 % kHandOver == 0, "");
 };
 static_assert(2 * (Few<128, 2>::kBytes + 1024) <= 233472, "two blocks per SM");
+// Spills (ptxas): heads of 128 with two row tiles 56 bytes stored, 80 loaded; the others none.
 
 // kFlat = false: grid (c, Hkv, S), clusters of c along x.  kFlat = true: a one-dimensional grid of shares.
 template <int D, int MT, bool kFlat>

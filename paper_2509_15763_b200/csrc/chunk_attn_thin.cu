@@ -8,6 +8,7 @@
 // Bound by reading K and V once.  (As rows of 128 the queries of drafted tokens cost four times the products, under the power limit;
 // as warp-level products twice the time of the memory.  64 sequences of 9216 slots, 1 to 8 tokens each: 432, 411 and 368 us.)
 // Work is dealt out as in the kernel for many rows: shares of all walks, parts of cut units added up by a second kernel.
+// Spills (ptxas): 8 bytes stored, 16 loaded.
 #include "chunk_walk.cuh"
 
 namespace ug {
