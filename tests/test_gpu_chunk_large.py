@@ -172,3 +172,67 @@ def test_the_largest_number_of_sequences_weighed_and_evicted():
             slots = evict_ref(w0[b, h, : int(lens[b])], int(lens[b]), keep, 2, 3)
             assert kept[b, h].tolist() == slots + [-1] * (keep - len(slots))
             assert torch.equal(w[b, h, : len(slots)].cpu(), w0[b, h][slots])
+
+
+@pytest.mark.parametrize("n,hq,dim,kernel", [(1, 8, 64, "chunk_few_kernel"), (3, 8, 128, "chunk_thin_sm100_kernel"), (70, 4, 64, "chunk_attn_sm100_kernel"),
+                                             (70, 4, 128, "chunk_attn_sm100_kernel")])
+def test_a_very_long_cache(n, hq, dim, kernel):
+    """400003 slots: attention and weights.  (Fewer bits than the slots have would show: the values of the far ones are large.)"""
+    L, scale = 400003, dim ** -0.5
+    cache = Cache([L], 1, dim, seed=1)
+    far = torch.zeros(cache.width * PG)
+    far[: L] = 1.0
+    far[: 700], far[L - 900: L - 100] = 30.0, 30.0
+    pages = cache.table[0, : cache.width].long()
+    cache.v[pages] = (cache.v[pages].float() * far.reshape(-1, 1, PG, 1)).to(torch.bfloat16)
+    q = (0.3 * torch.randn(n, hq, dim, generator=torch.Generator().manual_seed(2))).to(torch.bfloat16)
+    d, cu = cache.device(), cu_of([n]).to(DEV)
+    o, lse = torch.empty(n, hq, dim, dtype=torch.bfloat16, device=DEV), torch.empty(n, hq, device=DEV)
+    ws = attn_workspace(1, n, hq, 1, dim, cache.width)
+    names = launched(lambda: ug.unigist_chunk_attn(q.to(DEV), cu, d["k"], d["v"], d["table"], d["lens"], o, lse, ws))
+    assert names[0] == kernel
+    k, v = cache.rows(cache.k, 0).to(DEV)[0], cache.rows(cache.v, 0).to(DEV)[0]
+    want, want_lse, size = (torch.zeros(n, hq, dim, dtype=torch.float64), torch.zeros(n, hq, dtype=torch.float64), torch.zeros(n, hq, dim, dtype=torch.float64))
+    total = torch.zeros(L, dtype=torch.float64, device=DEV)
+    for i in range(n):
+        see = L - n + i + 1
+        z = q[i].double().to(DEV) @ k[:see].T * scale
+        l = torch.logsumexp(z, -1)
+        p = torch.exp(z - l[:, None])
+        total[:see] += p.sum(0)
+        want[i], want_lse[i], size[i] = (p @ v[:see]).cpu(), l.cpu(), (p @ v[:see].abs()).cpu()
+    check_attn(o, lse, (want, want_lse, size), kernel)
+    w = torch.zeros_like(d["w"])
+    ug.unigist_cache_weigh(q.to(DEV), cu, lse, d["k"], d["table"], d["lens"], None, w, 0.0)
+    ug.unigist_device_status()
+    got = cache.rows(w, 0)[0].to(DEV)
+    assert ((got - total).abs() - 3e-4 * total).max() <= 1e-30   # (1e-4 of the call itself, 2e-4 of the log-sum-exps that it was given)
+
+
+@pytest.mark.parametrize("keep,first,last", [(700, 4, 64), (150001, 0, 0), (1, 0, 0), (200002, 1, 1)])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("weights", ["random", "ties"])
+def test_eviction_from_a_cache_whose_weights_fit_no_cluster(keep, first, last, in_place, weights):
+    """More slots than the blocks of a cluster hold weights of: they are read again in every pass."""
+    L = 200003
+    cache = Cache([L, 100], 1, 64, seed=keep, waste=2.0, spare=1 + 2 * -(-keep // PG))
+    if weights == "ties":
+        cache.w = (cache.w * 3).round()
+    d = cache.device()
+    held = set(cache.table[0].tolist()) | {int(cache.table[1, 0]), int(cache.table[1, 1])}
+    width = -(-keep // PG)
+    fresh = torch.tensor([p for p in range(cache.blocks) if p not in held][: 2 * width], dtype=torch.int32).reshape(2, width)
+    to = d["table"] if in_place else fresh.to(DEV)
+    new_lens, kept = torch.zeros(2, dtype=torch.int32, device=DEV), torch.zeros(2, 1, keep, dtype=torch.int32, device=DEV)
+    names = launched(lambda: ug.unigist_cache_evict(d["k"], d["v"], d["w"], d["table"], d["lens"], to, new_lens, kept, keep, first, last))
+    assert names == ["evict_select_kernel", "evict_move_kernel"]
+    for b, n in enumerate((L, 100)):
+        m, w0 = min(n, keep), cache.rows(cache.w, b, n)[0]
+        number = torch.where(w0 > 0, w0, 0.0)
+        number[:first], number[n - last:] = float("inf"), float("inf")
+        want = torch.sort(number, descending=True, stable=True).indices[:m].sort().values if n > keep else torch.arange(n)
+        assert int(new_lens[b]) == m and torch.equal(kept[b, 0, :m].cpu().long(), want) and (kept[b, 0, m:] == -1).all()
+        for name in ("k", "v", "w"):
+            pages = to[b, : -(-m // PG)].cpu().long()
+            got = d[name].cpu()[pages, 0].flatten(0, 1)[:m]
+            assert torch.equal(got, getattr(cache, name)[cache.table[b, : -(-n // PG)].long(), 0].flatten(0, 1)[want])
