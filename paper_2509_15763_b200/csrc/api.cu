@@ -6,6 +6,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <mutex>
 
 #include "chunk.cuh"
 #include "ug_common.cuh"
@@ -106,6 +107,7 @@ struct TimeoutFlags {
   unsigned int* at[kFlags];
 };
 __device__ unsigned int g_timed_out;
+std::mutex g_status_lock;  // from the launch to the copy: another thread's launch between them would leave nothing to report
 __global__ void take_timeouts_kernel(TimeoutFlags flags) {
   const bool mine = threadIdx.x < kFlags && atomicExch(flags.at[threadIdx.x], 0u) != 0;
   const bool any = __any_sync(0xffffffffu, mine);
@@ -319,6 +321,7 @@ int32_t unigist_device_status(void) {
   TimeoutFlags flags;
   for (int i = 0; i < kFlags; ++i)
     if (int32_t rc = flag_of[i](&flags.at[i])) return rc;
+  const std::lock_guard<std::mutex> lock(g_status_lock);
   take_timeouts_kernel<<<1, 32>>>(flags);
   if (int32_t rc = check_launch("device status kernel")) return rc;
   unsigned int timed_out = 0;
