@@ -82,3 +82,45 @@ def test_eviction(lens, in_place):
         ug.unigist_cache_evict(o[0], o[1], o[2], v[0], v[1], v[0] if in_place else v[2], o[3], o[4], keep, 3, 5, stream=s)
 
     both([d["table"], d["lens"], to], [d["k"], d["v"], d["w"], torch.zeros_like(d["lens"]), torch.zeros(2, 2, keep, dtype=torch.int32, device=DEV)], call)
+
+
+@pytest.mark.parametrize("rows,dim,wide", [([5, 1, 3], 128, 0), ([5, 1, 3], 128, 400), ([3, 1, 2], 64, 400), ([90, 1, 40], 64, 0), ([90, 1, 40], 128, 0)])
+def test_a_whole_step_in_a_graph(rows, dim, wide):
+    """Rotation, append, attention, weights and eviction in place, one behind the other in a graph (whose kernels start before the one before
+    has ended): replayed three times, on what the last replay left, it is what the calls do by themselves."""
+    hq, hkv, keep, n = 8, 2, 150, sum(rows)
+    cache = Cache([500, 64, 170], hkv, dim, room=200, waste=1.0)
+    if wide:
+        table = torch.full((3, wide), -7, dtype=torch.int32)
+        table[:, : cache.width] = cache.table
+        cache.table, cache.width = table, wide
+    qkv, cu = rows_of(n, hq + 2 * hkv, dim), cu_of(rows).to(DEV)
+    pos = torch.arange(n, dtype=torch.int32, device=DEV)[None]
+    axes = [0] * (dim // 2)
+    states = []
+    for _ in range(2):
+        s = {**cache.device(), "q": torch.empty(n, hq, dim, dtype=torch.bfloat16, device=DEV), "lse": torch.empty(n, hq, device=DEV)}
+        s.update(o=torch.empty_like(s["q"]), longer=torch.zeros_like(s["lens"]), kept=torch.zeros(3, hkv, keep, dtype=torch.int32, device=DEV),
+                 ws=torch.empty(ug.unigist_chunk_attn_workspace_bytes(3, n, hq, hkv, dim, cache.width), dtype=torch.uint8, device=DEV))
+        states.append(s)
+
+    def step(s):
+        ug.unigist_rope_axes(qkv[:, :hq], s["q"], pos, axes, BASE)
+        ug.unigist_chunk_append(qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], cu, s["k"], s["v"], s["table"], s["lens"], s["longer"], s["w"], pos, axes, BASE)
+        ug.unigist_chunk_attn(s["q"], cu, s["k"], s["v"], s["table"], s["longer"], s["o"], s["lse"], s["ws"])
+        ug.unigist_cache_weigh(s["q"], cu, s["lse"], s["k"], s["table"], s["longer"], s["w"], s["w"], 0.9)
+        ug.unigist_cache_evict(s["k"], s["v"], s["w"], s["table"], s["longer"], s["table"], s["lens"], s["kept"], keep, 4, 20)
+
+    eager, captured = states
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for _ in range(3):
+        step(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in ("q", "o", "lse", "longer", "kept", "lens", "k", "v", "w"):
+            assert torch.equal(eager[name], captured[name]), name
+        assert torch.isfinite(eager["o"].float()).all() and eager["lens"].max() <= keep
+    ug.unigist_device_status()
